@@ -8,8 +8,9 @@
 //    second product as they stand, for rows 4 (lane / 32) + 0..3 (+ 8) of every 16: the A operand takes V's rows in that order.
 //  * K and V go from memory straight into LDS, a tile ahead.  Eight rows in a row lie in one page (pages are powers of two from 8 rows on), so page numbers are
 //    looked up through the scalar cache, and an address is a wave-uniform base plus a lane's fixed offset.
-//  * The maximum is only moved, and the sums rescaled, when a score exceeds it by more than 2^8: a probability may be up to 256 until then, which fp32 sums and
-//    binary16 operands hold as well as one up to 1.
+//  * The maximum is only moved, and the sums rescaled, when a probability would exceed the largest so far by a factor (TreeRange): fp32 sums hold those as well as ones up to 1.
+//  * Probabilities that become binary16 numbers are relative to the maximum times 2^12, which the quotient with their sum cancels: rows far below the maximum, which may be
+//    many (behind a first token that takes nearly everything, say), would else be subnormal numbers of few bits, or zero from 2^-25 of the largest on.
 //  * fp32 queries: Q (scaled by a power of two per query) and P as two binary16 numbers each, 22 bits, two products into one accumulator.
 //  * Tiles with drafted rows, rows past the end or rows whose page is absent are special: scores are masked by selection, and V's rows that nobody sees are
 //    zeroed in LDS (zero times what they hold need not be zero).  A drafted row that somebody sees and another does not may hold infinities or NaN: such elements are
@@ -32,7 +33,17 @@ typedef short s4v __attribute__((ext_vector_type(4)));
 constexpr int TREE_MAX_RANGES = 256;
 constexpr int TREE_STEP = 64;        // rows that ranges are multiples of
 constexpr int TREE_REC = 4;          // a record: (maximum, sum, -, -), D columns
-constexpr float TREE_DEFER = 8.f;    // in powers of two
+
+// Of the probabilities that enter the products as numbers of type C, in powers of two: LIFT is what the largest score so far has, DEFER how far above it one may be before the
+// maximum is moved.  Binary16 ends below 2^16; 2^3 is passed by hardly any score behind the first tile's (N(0, 1) scores: maxima of 64 and 6000 are 2.4 and 3.8).  bfloat16 has fp32's range.
+template <class C>
+struct TreeRange {
+    static constexpr float LIFT = 12.f, DEFER = 3.f;
+};
+template <>
+struct TreeRange<BF16> {
+    static constexpr float LIFT = 0.f, DEFER = 8.f;
+};
 
 struct TreeAttnArgs {
     PagedArgs p;
@@ -389,7 +400,7 @@ __global__ void __launch_bounds__(512, 2) tree_wide_kernel(TreeAttnArgs a)
         for (int x = 0; x < STEPS; ++x) split8(qv[x], s, qh[x], ql[x]);
     }
 
-    float m = -INFINITY, mf = 0.f, l = 0.f; // maximum of the scores before f, m f (0: there is none yet), this lane's half of the sum
+    float m = -INFINITY, mf = 0.f, l = 0.f; // maximum of the scores before f, m f - LIFT (0: there is none yet), this lane's half of the sum
     f16v acc[DB], s[BLOCKS];
 #pragma unroll
     for (int x = 0; x < DB; ++x)
@@ -479,9 +490,9 @@ __global__ void __launch_bounds__(512, 2) tree_wide_kernel(TreeAttnArgs a)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[k][e]);
         top = max_across_32(top);
-        // (nothing to see yet: m f is 0 and the first score there is moves it, whatever it is)
-        if (__ballot(m == -INFINITY ? top > m : top * f > mf + TREE_DEFER) != 0) {
-            const float mn = fmaxf(m, top), mnf = mn == -INFINITY ? 0.f : mn * f;
+        // (nothing to see yet: mf is 0 and the first score there is moves it, whatever it is)
+        if (__ballot(m == -INFINITY ? top > m : fmaf(top, f, -mf) > TreeRange<C>::LIFT + TreeRange<C>::DEFER) != 0) {
+            const float mn = fmaxf(m, top), mnf = mn == -INFINITY ? 0.f : fmaf(mn, f, -TreeRange<C>::LIFT);
             const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mf - mnf); // (nothing so far: the sums are 0)
             l *= corr;
 #pragma unroll
@@ -795,7 +806,7 @@ __global__ void __launch_bounds__(256, 2) tree_narrow_kernel(TreeAttnArgs a)
     }
 
     bool odd = false; // this lane has met infinities or NaN in drafted rows
-    float m[NQ], mf[NQ], l[NQ]; // maximum of the scores before f, m f (0: there is none yet), this lane's quarter of the sum
+    float m[NQ], mf[NQ], l[NQ]; // maximum of the scores before f, m f - LIFT (0: there is none yet), this lane's quarter of the sum
     f4v acc[NQ][DB];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -851,9 +862,9 @@ __global__ void __launch_bounds__(256, 2) tree_narrow_kernel(TreeAttnArgs a)
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const float top = max_across_32(max_across_16(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3]))));
-            // (nothing to see yet: m f is 0 and the first score there is moves it, whatever it is)
-            if (__ballot(m[n] == -INFINITY ? top > m[n] : top * f[n] > mf[n] + TREE_DEFER) != 0) {
-                const float mn = fmaxf(m[n], top), mnf = mn == -INFINITY ? 0.f : mn * f[n];
+            // (nothing to see yet: mf is 0 and the first score there is moves it, whatever it is)
+            if (__ballot(m[n] == -INFINITY ? top > m[n] : fmaf(top, f[n], -mf[n]) > TreeRange<C>::LIFT + TreeRange<C>::DEFER) != 0) {
+                const float mn = fmaxf(m[n], top), mnf = mn == -INFINITY ? 0.f : fmaf(mn, f[n], -TreeRange<C>::LIFT);
                 const float corr = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mf[n] - mnf); // (nothing so far: the sums are 0)
                 l[n] *= corr;
 #pragma unroll
