@@ -487,7 +487,8 @@ prima_status prima_rope_table(int32_t n_rows, int32_t head_dim, float theta, flo
  * A token that sees no row, or none whose score is above -infinity, gets zeros.  Rows that a token does not see may hold anything, infinities
  * and NaN included.  An infinity in V of a row that it sees leaves nothing finite in its column: infinity, or NaN where a probability that enters
  * the product is zero (with fp32 queries: where one of its two parts is).  Scores, maxima and sums are fp32.  With fp32 queries the probabilities and the queries enter
- * the matrix cores as two binary16 numbers each (errors as of fp32 arithmetic), else the probabilities are rounded to the cache's type.
+ * the matrix cores as two binary16 numbers each (errors as of fp32 arithmetic).  With queries of the cache's type probabilities are two numbers of it, or, where many
+ * queries share a KV head (never with up to 32), rounded to one.
  * workspace: prima_tree_attn_workspace_bytes(pages, step, n_q_heads) bytes (0 for arguments the call would refuse), 256-byte aligned.
  */
 prima_status prima_tree_attn(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype,

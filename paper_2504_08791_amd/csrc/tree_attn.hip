@@ -11,7 +11,8 @@
 //  * The maximum is only moved, and the sums rescaled, when a probability would exceed the largest so far by a factor (TreeRange): fp32 sums hold those as well as ones up to 1.
 //  * Probabilities that become binary16 numbers are relative to the maximum times 2^12, which the quotient with their sum cancels: rows far below the maximum, which may be
 //    many (behind a first token that takes nearly everything, say), would else be subnormal numbers of few bits, or zero from 2^-25 of the largest on.
-//  * fp32 queries: Q (scaled by a power of two per query) and P as two binary16 numbers each, 22 bits, two products into one accumulator.
+//  * fp32 queries: Q (scaled by a power of two per query) and P as two binary16 numbers each, 22 bits, two products into one accumulator.  16-bit queries: P as two numbers of
+//    the type where few queries wait for the rows anyway, rounded to one where many make the products the bound.
 //  * Tiles with drafted rows, rows past the end or rows whose page is absent are special: scores are masked by selection, and V's rows that nobody sees are
 //    zeroed in LDS (zero times what they hold need not be zero).  A drafted row that somebody sees and another does not may hold infinities or NaN: such elements are
 //    zeroed for the product and added to the sums of those that see them in the end.
@@ -516,6 +517,9 @@ __global__ void __launch_bounds__(512, 2) tree_wide_kernel(TreeAttnArgs a)
             for (int e = 0; e < 16; ++e) l += s[k][e];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
+                // 16-bit queries: probabilities rounded to the cache's type, as the output is in the end: its error against 64 bits is 1.4 times that of the output's rounding alone
+                // (2.34e-3 of the rms instead of 1.66e-3 in bf16, 2.9e-4 instead of 2.1e-4 in f16).  Two numbers, as with fp32 queries, leave that alone but are half as many
+                // products again: 8 x 63 bf16 tokens behind 6000 rows 99 -> 127 us, 8 x 20 51 -> 62.
                 if constexpr (__is_same(C, BF16)) {
                     b8 hi;
 #pragma unroll
@@ -674,6 +678,37 @@ __device__ __forceinline__ f4v tree_mfma16_half(s4v a, s4v b, f4v c)
     typedef _Float16 h4 __attribute__((ext_vector_type(4)));
     if constexpr (__is_same(C, BF16)) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(h4, a), __builtin_bit_cast(h4, b), c, 0, 0, 0);
+}
+
+// Probabilities as two numbers of type C, whatever the queries' type: the stream of rows hides the second product (us, rounded once / in two: 16 sequences of one f16 token behind 4100 rows
+// 44.2 / 44.7, one behind 30001 26.4 / 26.9, 36 of 4 bf16 tokens behind 3000 72.3 / 74.9).  The first is cut off, not rounded, and the second is above zero where the probability is: an
+// infinity in V then stays one.
+template <class C>
+__device__ __forceinline__ void split_probabilities(const float (&p)[4], s4v &hi, s4v &lo)
+{
+    typedef typename C::type C4 __attribute__((ext_vector_type(4)));
+    C4 l;
+    if constexpr (__is_same(C, BF16)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const unsigned cut = __builtin_bit_cast(unsigned, p[r]) & 0xffff0000u;
+            hi[r] = static_cast<short>(cut >> 16);
+            l[r] = static_cast<__bf16>(fmaxf(p[r] - __builtin_bit_cast(float, cut), p[r] * 0x1p-24f));
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+            typedef short s2v __attribute__((ext_vector_type(2)));
+            const auto cut = __builtin_amdgcn_cvt_pkrtz(p[r], p[r + 1]);
+            const s2v bits = __builtin_bit_cast(s2v, cut); // (of the pair: the compiler takes the first for either of its elements)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                hi[r + e] = bits[e];
+                l[r + e] = static_cast<_Float16>(__builtin_amdgcn_fmed3f(p[r + e] - static_cast<float>(cut[e]), 0x1p-24f, p[r + e])); // (2^-24: the least binary16 number)
+            }
+        }
+    }
+    lo = __builtin_bit_cast(s4v, l);
 }
 
 template <class A, class C, int D, int NQ>
@@ -879,23 +914,7 @@ __global__ void __launch_bounds__(256, 2) tree_narrow_kernel(TreeAttnArgs a)
                 if (special) p[r] = sees[n] >> (4 * g + r) & 1 ? p[r] : 0.f;
                 l[n] += p[r];
             }
-            if constexpr (__is_same(C, BF16)) {
-                typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-                b4 hi;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) hi[r] = static_cast<__bf16>(p[r]);
-                ph[n] = __builtin_bit_cast(s4v, hi);
-            } else {
-                typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-                h4 hi, lo;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    hi[r] = static_cast<_Float16>(p[r]);
-                    if constexpr (SPLIT) lo[r] = static_cast<_Float16>(p[r] - static_cast<float>(hi[r]));
-                }
-                ph[n] = __builtin_bit_cast(s4v, hi);
-                if constexpr (SPLIT) pl[n] = __builtin_bit_cast(s4v, lo);
-            }
+            split_probabilities<C>(p, ph[n], pl[n]);
         }
         if (i + 2 < n_tiles) wait_loads<3 * NI>();
         else if (i + 1 < n_tiles) wait_loads<2 * NI>();
@@ -923,7 +942,7 @@ __global__ void __launch_bounds__(256, 2) tree_narrow_kernel(TreeAttnArgs a)
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 acc[n][x] = tree_mfma16_half<C>(v[x], ph[n], acc[n][x]);
-                if constexpr (SPLIT) acc[n][x] = tree_mfma16_half<C>(v[x], pl[n], acc[n][x]);
+                acc[n][x] = tree_mfma16_half<C>(v[x], pl[n], acc[n][x]);
             }
         if (i + 2 < n_tiles) request(i + 2, after, 1);
         now = next;
