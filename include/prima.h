@@ -488,13 +488,18 @@ prima_status prima_rope_table(int32_t n_rows, int32_t head_dim, float theta, flo
  * and NaN included.  An infinity in V of a row that it sees leaves nothing finite in its column: infinity, or NaN where a probability that enters
  * the product is zero (with fp32 queries: where one of its two parts is).  Scores, maxima and sums are fp32.  With fp32 queries the probabilities and the queries enter
  * the matrix cores as two binary16 numbers each (errors as of fp32 arithmetic).  With queries of the cache's type probabilities are two numbers of it, or, where many
- * queries share a KV head (never with up to 32), rounded to one.
+ * queries share a KV head (prima_tree_attn_plan: the kernel for many), rounded to one.
  * workspace: prima_tree_attn_workspace_bytes(pages, step, n_q_heads) bytes (0 for arguments the call would refuse), 256-byte aligned.
  */
 prima_status prima_tree_attn(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype,
                              const void *q, int64_t ldq, float scale, void *o, int64_t ldo,
                              void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t prima_tree_attn_workspace_bytes(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads);
+/* Host only: how that call shares the step out.  few, many: queries (tokens times heads of a group) of a workgroup, in blocks of 16 of the kernel for few of them or of 32 of the
+ * one for many; the other is 0 (both: no tokens).  ranges, range_rows: HOST [n_seqs]: into how many ranges a sequence's rows are divided (0: no tokens) and how many rows each has but
+ * the last. */
+prima_status prima_tree_attn_plan(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype, int32_t *few, int32_t *many,
+                                  int32_t *ranges, int32_t *range_rows);
 
 /*
  * The accepted branch of every sequence's tree moved to its place, in all layers: row n_past[b] + path[b*ld_path + i] becomes row n_past[b] + i,

@@ -10,7 +10,8 @@ import torch
 from . import _ffi
 from ._ffi import Dims, Layer, PrimaError, MAX_TOK  # noqa: F401
 from .paged import (BEAM_MAX, PAGED_MAX_SEQS, TREE_MAX_TOK, PagedCache, PagedStep, beam_reorder, beam_select,  # noqa: F401
-                    beam_select_workspace_bytes, draft_tree, paged_append, rope_table, tree_accept, tree_attn, tree_attn_workspace_bytes)
+                    beam_select_workspace_bytes, draft_tree, paged_append, rope_table, tree_accept, tree_attn, tree_attn_plan,
+                    tree_attn_workspace_bytes)
 
 _WEIGHTS = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown")
 

@@ -22,7 +22,7 @@ EXPORTS = ["prima_q4k_gemv", "prima_gemv_workspace_bytes", "prima_q4k_dequant", 
            "prima_q4k_gemm", "prima_gemm_workspace_bytes", "prima_gemm_workspace_bytes_ksplit", "prima_gemm_ksplit", "prima_layer_window_prefill", "prima_prefill_workspace_bytes",
            "prima_layer_window_prefill_mixed", "prima_set_prefill_small_tokens", "prima_q4k_gemv_noalloc",
            "prima_gguf_tensor_bytes", "prima_repack_gguf", "prima_fmt_gemm_plan",
-           "prima_paged_append", "prima_rope_table", "prima_tree_attn", "prima_tree_attn_workspace_bytes", "prima_tree_accept",
+           "prima_paged_append", "prima_rope_table", "prima_tree_attn", "prima_tree_attn_workspace_bytes", "prima_tree_attn_plan", "prima_tree_accept",
            "prima_beam_select", "prima_beam_select_workspace_bytes", "prima_beam_reorder"]
 FORMATS = {"q4_k": 0, "q5_k": 1, "q6_k": 2, "q8_0": 3, "f16": 4, "f32": 5}
 
@@ -145,12 +145,13 @@ def lib():
         L.prima_tree_attn.argtypes = [pp, sp, i32, i32, vp, i64, C.c_float, vp, i64, vp, sz, vp]
         L.prima_tree_attn_workspace_bytes.argtypes = [pp, sp, i32]
         L.prima_tree_attn_workspace_bytes.restype = sz
+        L.prima_tree_attn_plan.argtypes = [pp, sp, i32, i32] + [C.POINTER(i32)] * 4
         L.prima_tree_accept.argtypes = [pp, i64, i32, sp, vp, i32, vp, vp]
         L.prima_beam_select.argtypes = [i32, vp, i64, i32, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
         L.prima_beam_select_workspace_bytes.argtypes = [i32, i32, i64, i32]
         L.prima_beam_select_workspace_bytes.restype = sz
         L.prima_beam_reorder.argtypes = [pp, i64, i32, i32, i32, C.POINTER(i32), vp, vp, vp, i32, vp]
-        for name in ("prima_paged_append", "prima_rope_table", "prima_tree_attn", "prima_tree_accept", "prima_beam_select", "prima_beam_reorder"):
+        for name in ("prima_paged_append", "prima_rope_table", "prima_tree_attn", "prima_tree_attn_plan", "prima_tree_accept", "prima_beam_select", "prima_beam_reorder"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib

@@ -1274,6 +1274,24 @@ size_t prima_tree_attn_workspace_bytes(const prima_kv_pages *pages, const prima_
     return split > whole ? split : whole; // (whatever the queries' type)
 }
 
+prima_status prima_tree_attn_plan(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype, int32_t *few, int32_t *many,
+                                  int32_t *ranges, int32_t *range_rows)
+{
+    if (!few || !many || !ranges || !range_rows) return PRIMA_E_NULL;
+    TreeAttnArgs a{};
+    const prima_status s = paged_args(pages, step, a.p);
+    if (s != PRIMA_OK) return s;
+    if (!act_dtype_ok(*pages, dtype) || !tree_heads_ok(n_q_heads, a.p.Hkv)) return PRIMA_E_SHAPE;
+    const TreePlan r = tree_plan(a.p, n_q_heads, pages->head_dim, dtype == PRIMA_DT_F32, a);
+    *few = r.narrow;
+    *many = r.wide;
+    for (int b = 0; b < a.p.n_seqs; ++b) {
+        ranges[b] = a.ranges[b];
+        range_rows[b] = a.range_rows[b];
+    }
+    return PRIMA_OK;
+}
+
 prima_status prima_tree_attn(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype, const void *q, int64_t ldq,
                              float scale, void *o, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream)
 {

@@ -162,6 +162,15 @@ def tree_attn_workspace_bytes(cache, step, n_heads):
     return _ffi.lib().prima_tree_attn_workspace_bytes(cache._refs[0], step._ref, n_heads)
 
 
+def tree_attn_plan(cache, step, n_heads, dtype):
+    """How tree_attn shares the step out: (few, many, ranges, range_rows), queries of a workgroup in blocks of 16 or of 32 (the kernel that is not used: 0) and,
+    per sequence, the ranges its rows are divided into and how many rows each has but the last."""
+    few, many, B = C.c_int32(), C.c_int32(), step.n_seqs
+    ranges, rows = (C.c_int32 * max(B, 1))(), (C.c_int32 * max(B, 1))()
+    _ffi.check(_ffi.lib().prima_tree_attn_plan(cache._refs[0], step._ref, n_heads, _DTYPES[dtype], C.byref(few), C.byref(many), ranges, rows), "prima_tree_attn_plan")
+    return few.value, many.value, list(ranges)[:B], list(rows)[:B]
+
+
 def tree_attn(cache, layer, step, q, o=None, scale=None, workspace=None):
     """Attention of the step's tokens q [tokens, heads, D] over their sequences' rows in the pages of `layer`, the step's own (appended before)
     among them -> o like q.  scale: None: D ** -0.5."""

@@ -126,3 +126,35 @@ def test_draft_tree():
     for bad in ([0], [-1, 1], [-2], [-1] * 65):
         with pytest.raises(ValueError):
             draft_tree(bad)
+
+
+def _plan(pages=None, step=None, heads=4, dtype=0):
+    p, s = pages or _pages(), step or _step()
+    n = s.n_seqs
+    few, many, ranges, rows = C.c_int32(-1), C.c_int32(-1), (C.c_int32 * max(n, 1))(), (C.c_int32 * max(n, 1))()
+    code = _ffi.lib().prima_tree_attn_plan(C.byref(p), C.byref(s), heads, dtype, C.byref(few), C.byref(many), ranges, rows)
+    return code, few.value, many.value, list(ranges)[:n], list(rows)[:n]
+
+
+def test_attention_plans():
+    """Host logic, no GPU: which kernel a step goes to, and ranges that cover every sequence's rows, each of which has some."""
+    seen = set()
+    for Hkv, G in ((1, 1), (2, 5), (8, 4), (8, 8), (1, 64)):
+        pages = _pages(n_kv_heads=Hkv, page_rows=64, head_stride=64 * 128, page_stride=Hkv * 64 * 128)
+        for dtype in (0, 1):
+            for tok in (1, 3, 7, 16, 33, 63):
+                for n in (1, 5, 64):
+                    for past in (0, 63, 500, 7001, 50000):
+                        pasts, toks = [past - past * b // (3 * n) for b in range(n)], [tok - (b % 3) * tok // 3 if b else tok for b in range(n)]
+                        code, few, many, ranges, rows = _plan(pages, _step(n_past=pasts, n_tok=toks, table_stride=1000), Hkv * G, dtype)
+                        assert code == 0 and (few in (1, 2) and many == 0 or few == 0 and many in ((2, 4) if dtype == 0 else (2, 4, 8)))
+                        assert few or tok * G > 32
+                        for p, t, k, r in zip(pasts, toks, ranges, rows):
+                            assert (k == 0) if t == 0 else (1 <= k <= 256 and r % 64 == 0 and (k - 1) * r < p + t <= k * r)
+                        seen.add((few, many))
+    assert seen == {(1, 0), (2, 0), (0, 2), (0, 4), (0, 8)}
+    assert _plan(step=_step(n_tok=(0,)))[:4] == (0, 0, 0, [0])
+    assert _plan(pages=_pages(dtype=0))[0] == 2 and _plan(heads=3)[0] == 2 and _plan(dtype=2)[0] == 2 and _plan(step=_step(n_tok=(65,)))[0] == 4
+    p, s, x = _pages(), _step(), C.c_int32()
+    for null in range(4):
+        assert _ffi.lib().prima_tree_attn_plan(C.byref(p), C.byref(s), 4, 0, *(None if i == null else C.byref(x) for i in range(4))) == 1
