@@ -179,7 +179,7 @@ __device__ __forceinline__ TreeWork tree_work(const TreeAttnArgs &a, int lane)
     w.range = (Hkv & (Hkv - 1)) == 0 ? unit >> __builtin_ctz(Hkv) : unit / Hkv;
     w.kvh = unit - w.range * Hkv;
     w.row0 = w.range * each;
-    w.row1 = min(w.row0 + each, w.past + w.n_tok);
+    w.row1 = w.row0 + min(each, w.past + w.n_tok - w.row0); // (the last range's end need not be a 32-bit number)
     return w;
 }
 
@@ -1154,12 +1154,12 @@ static TreePlan tree_plan(const PagedArgs &p, int Hq, int D, bool split, TreeAtt
         int64_t n = 0;
         for (int b = 0; b < p.n_seqs; ++b) {
             const int tok = p.tok0[b + 1] - p.tok0[b];
-            if (tok) n += static_cast<int64_t>((p.n_past[b] + tok + rows - 1) / rows) * tiles_of(tok);
+            if (tok) n += (static_cast<int64_t>(p.n_past[b]) + tok + rows - 1) / rows * tiles_of(tok);
         }
         return n * p.Hkv;
     };
     int lo = 1, hi = (most_rows + TREE_STEP - 1) / TREE_STEP; // steps of a range: the fewest that fit
-    const int least = (most_rows + TREE_STEP * TREE_MAX_RANGES - 1) / (TREE_STEP * TREE_MAX_RANGES);
+    const int least = static_cast<int>((static_cast<int64_t>(most_rows) + TREE_STEP * TREE_MAX_RANGES - 1) / (TREE_STEP * TREE_MAX_RANGES));
     if (lo < least) lo = least;
     if (most_rows <= 256) lo = hi;
     while (lo < hi) {

@@ -158,3 +158,16 @@ def test_attention_plans():
     p, s, x = _pages(), _step(), C.c_int32()
     for null in range(4):
         assert _ffi.lib().prima_tree_attn_plan(C.byref(p), C.byref(s), 4, 0, *(None if i == null else C.byref(x) for i in range(4))) == 1
+
+
+@pytest.mark.parametrize("Hkv,G", [(1, 1), (1, 60), (8, 8), (600, 1)])
+@pytest.mark.parametrize("tok", [1, 64])
+def test_attention_plans_of_the_longest_sequences(Hkv, G, tok):
+    """Up to the most cached rows that a step may name, 2^31 - 1 - 1024 - 64: ranges, which end behind 32 bits, cover all rows."""
+    pages = _pages(n_kv_heads=Hkv, page_rows=1024, head_stride=1024 * 128, page_stride=Hkv * 1024 * 128)
+    for past in (2 ** 31 - 1089, 2 ** 31 - 2000, 2 ** 31 - 16400, 2 ** 30):
+        code, few, many, ranges, rows = _plan(pages, _step(n_past=(past, 10), n_tok=(tok, 0), table_stride=2 ** 21), Hkv * G, 0)
+        assert code == 0 and bool(few) != bool(many) and ranges[1] == 0
+        assert 1 <= ranges[0] <= 256 and 0 < rows[0] and (ranges[0] - 1) * rows[0] < past + tok <= ranges[0] * rows[0]
+        if Hkv == 1 and G == 1:
+            assert ranges[0] > 128 and (past < 2 ** 31 - 2000 or ranges[0] * rows[0] >= 2 ** 31)
