@@ -489,7 +489,7 @@ prima_status prima_rope_table(int32_t n_rows, int32_t head_dim, float theta, flo
  * the product is zero (with fp32 queries: where one of its two parts is).  Scores, maxima and sums are fp32.  With fp32 queries the probabilities and the queries enter
  * the matrix cores as two binary16 numbers each (errors as of fp32 arithmetic).  With queries of the cache's type probabilities are two numbers of it, or, where many
  * queries share a KV head (prima_tree_attn_plan: the kernel for many), rounded to one.
- * workspace: prima_tree_attn_workspace_bytes(pages, step, n_q_heads) bytes (0 for arguments the call would refuse), 256-byte aligned.
+ * workspace: prima_tree_attn_workspace_bytes(pages, step, n_q_heads) bytes (at least 256; 0 only for arguments the call would refuse), 256-byte aligned.
  */
 prima_status prima_tree_attn(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype,
                              const void *q, int64_t ldq, float scale, void *o, int64_t ldo,

@@ -1271,7 +1271,8 @@ size_t prima_tree_attn_workspace_bytes(const prima_kv_pages *pages, const prima_
     TreeAttnArgs a{};
     if (paged_args(pages, step, a.p) != PRIMA_OK || !tree_heads_ok(n_q_heads, a.p.Hkv)) return 0;
     const size_t split = tree_plan(a.p, n_q_heads, pages->head_dim, true, a).bytes, whole = tree_plan(a.p, n_q_heads, pages->head_dim, false, a).bytes;
-    return split > whole ? split : whole; // (whatever the queries' type)
+    const size_t most = split > whole ? split : whole; // (whatever the queries' type)
+    return most > 256 ? most : 256;                    // (none are needed: some all the same, since 0 is what a refusal gives and the call takes no null pointer)
 }
 
 prima_status prima_tree_attn_plan(const prima_kv_pages *pages, const prima_paged_step *step, int32_t n_q_heads, int32_t dtype, int32_t *few, int32_t *many,

@@ -171,3 +171,17 @@ def test_attention_plans_of_the_longest_sequences(Hkv, G, tok):
         assert 1 <= ranges[0] <= 256 and 0 < rows[0] and (ranges[0] - 1) * rows[0] < past + tok <= ranges[0] * rows[0]
         if Hkv == 1 and G == 1:
             assert ranges[0] > 128 and (past < 2 ** 31 - 2000 or ranges[0] * rows[0] >= 2 ** 31)
+
+
+def test_attention_scratch_is_never_nothing_for_a_call_that_is_taken():
+    """A caller that allocates what it is told has something to pass; 0 is for what is refused."""
+    size = lambda pages, step, heads: _ffi.lib().prima_tree_attn_workspace_bytes(C.byref(pages), C.byref(step), heads)
+    for step in (_step(), _step(n_past=(0,), n_tok=(1,)), _step(n_tok=(0,)), _step(n_past=(40, 0), n_tok=(0, 0))):
+        assert size(_pages(), step, 4) == 256 and _attn(step=_step(n_tok=(0,)), n=256) == 0
+    long = _step(n_past=(5000,), table_stride=400)
+    need = size(_pages(), long, 4)
+    ranges = _plan(step=long)[3][0]
+    assert ranges > 1 and need >= 3 * 4 * ranges * (4 + 128) * 4 and need % 256 == 0
+    assert _attn(step=long, n=need - 256) == 5
+    for pages, step, heads in ((_pages(dtype=0), _step(), 4), (_pages(), _step(n_tok=(65,)), 4), (_pages(), _step(), 3), (_pages(), _step(n_past=None), 4), (_pages(k=None), _step(), 4)):
+        assert size(pages, step, heads) == 0
