@@ -12,6 +12,7 @@ torch CUDA tensors go to the C ABI of include/prima.h, all computation happens i
     table = beam_reorder(cache, table, beams, n_rows)     # all layers
 """
 import ctypes as C
+from threading import get_ident
 
 import torch
 
@@ -81,7 +82,8 @@ class PagedStep:
     tree    int64 [tokens] or None: bit j: the token attends to its sequence's drafted token j (draft_tree makes them; its own bit among
             them).  None: chains
     positions   int32 [tokens] or None: where a token is rotated to.  None: n_past + its index
-    Keeps the tensors alive, and the scratch that tree_attn takes where it is given none, one per stream, for the layers that follow."""
+    Keeps the tensors alive, and the scratch that tree_attn takes where it is given none, for the layers that follow: one per thread and stream, since a call enqueues two
+    launches, between which another thread's may come."""
 
     def __init__(self, n_past, n_tok, table, tree=None, positions=None):
         B = len(n_past)
@@ -186,7 +188,7 @@ def tree_attn(cache, layer, step, q, o=None, scale=None, workspace=None):
         return o
     stream = _stream(q)
     if workspace is None:  # a step's calls have the same need for every layer of a cache; a graph gets scratch of its own
-        key = (stream, heads, D, cache.n_kv_heads)
+        key = (get_ident(), stream, heads, D, cache.n_kv_heads)
         capturing = torch.cuda.is_current_stream_capturing()
         workspace = None if capturing else step._scratch.get(key)
         if workspace is None:
