@@ -1203,41 +1203,50 @@ static TreePlan tree_plan(const PagedArgs &p, int Hq, int D, bool split, TreeAtt
     return r;
 }
 
-static prima_status launch_tree(const void *kernel, int threads, size_t lds, std::atomic<bool> &attr_set, dim3 grid, TreeAttnArgs a, hipStream_t st)
+// The kernels' dynamic LDS may pass 64 KiB: all of them are told on the first call, whichever it launches, so that a step of other lengths, heads or types may be captured after it.
+template <class A, class C, int D>
+static bool tree_attributes()
 {
-    if (!attr_set) { // set twice by two threads at worst: the attribute call is idempotent
-        if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds)) != hipSuccess) return PRIMA_E_DEVICE;
-        attr_set = true;
-    }
-    void *args[] = {&a};
-    return hipLaunchKernel(kernel, grid, dim3(threads), args, lds, st) == hipSuccess ? PRIMA_OK : PRIMA_E_DEVICE;
+    auto set = [](auto kernel, size_t lds) {
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds)) == hipSuccess;
+    };
+    bool ok = set(tree_narrow_kernel<A, C, D, 1>, TreeNarrow<A, D, 1>::LDS) && set(tree_narrow_kernel<A, C, D, 2>, TreeNarrow<A, D, 2>::LDS) &&
+              set(tree_wide_kernel<A, C, D, 2>, TreeShape<D, 2>::LDS) && set(tree_wide_kernel<A, C, D, 4>, TreeShape<D, 4>::LDS);
+    if constexpr (!__is_same(A, F32)) ok = ok && set(tree_wide_kernel<A, C, D, 8>, TreeShape<D, 8>::LDS); // (no plan has it with fp32 queries)
+    return ok;
+}
+static bool tree_attributes_set()
+{
+    static std::atomic<bool> done{false};
+    if (!done) // set twice by two threads at worst: the attribute calls are idempotent
+        done = tree_attributes<F32, F16, 128>() && tree_attributes<F16, F16, 128>() && tree_attributes<BF16, BF16, 128>() && tree_attributes<F32, F16, 64>() &&
+               tree_attributes<F16, F16, 64>() && tree_attributes<BF16, BF16, 64>();
+    return done;
 }
 
 template <class A, class C, int D, int NQ>
-static prima_status launch_tree_narrow(const TreeAttnArgs &a, dim3 grid, hipStream_t st)
+static void launch_tree_narrow(const TreeAttnArgs &a, dim3 grid, hipStream_t st)
 {
-    static std::atomic<bool> attr_set{false};
-    return launch_tree(reinterpret_cast<const void *>(tree_narrow_kernel<A, C, D, NQ>), 256, TreeNarrow<A, D, NQ>::LDS, attr_set, grid, a, st);
+    hipLaunchKernelGGL((tree_narrow_kernel<A, C, D, NQ>), grid, dim3(256), (TreeNarrow<A, D, NQ>::LDS), st, a);
 }
 template <class A, class C, int D, int NR>
-static prima_status launch_tree_wide(const TreeAttnArgs &a, dim3 grid, hipStream_t st)
+static void launch_tree_wide(const TreeAttnArgs &a, dim3 grid, hipStream_t st)
 {
-    static std::atomic<bool> attr_set{false};
-    return launch_tree(reinterpret_cast<const void *>(tree_wide_kernel<A, C, D, NR>), 512, TreeShape<D, NR>::LDS, attr_set, grid, a, st);
+    hipLaunchKernelGGL((tree_wide_kernel<A, C, D, NR>), grid, dim3(512), (TreeShape<D, NR>::LDS), st, a);
 }
 
 template <class A, class C, int D>
 static prima_status launch_tree_attn(const TreeAttnArgs &a, const TreePlan &r, hipStream_t st)
 {
     const dim3 grid(r.groups);
-    prima_status s;
-    if (r.narrow == 1) s = launch_tree_narrow<A, C, D, 1>(a, grid, st);
-    else if (r.narrow == 2) s = launch_tree_narrow<A, C, D, 2>(a, grid, st);
-    else if (r.wide == 2) s = launch_tree_wide<A, C, D, 2>(a, grid, st);
-    else if (r.wide == 4) s = launch_tree_wide<A, C, D, 4>(a, grid, st);
-    else if constexpr (!__is_same(A, F32)) s = launch_tree_wide<A, C, D, 8>(a, grid, st);
-    else s = PRIMA_E_DEVICE; // (no plan has it)
-    if (s != PRIMA_OK || r.most < 2) return s;
+    if (!tree_attributes_set()) return PRIMA_E_DEVICE;
+    if (r.narrow == 1) launch_tree_narrow<A, C, D, 1>(a, grid, st);
+    else if (r.narrow == 2) launch_tree_narrow<A, C, D, 2>(a, grid, st);
+    else if (r.wide == 2) launch_tree_wide<A, C, D, 2>(a, grid, st);
+    else if (r.wide == 4) launch_tree_wide<A, C, D, 4>(a, grid, st);
+    else if constexpr (!__is_same(A, F32)) launch_tree_wide<A, C, D, 8>(a, grid, st);
+    else return PRIMA_E_DEVICE; // (no plan has it)
+    if (r.most < 2) return last_launch_status();
     constexpr int few = 1024 / D; // queries of a workgroup
     const dim3 groups((a.Hq + few - 1) / few, paged_tokens(a.p));
     if (r.most <= 2) hipLaunchKernelGGL((tree_join_few_kernel<A, D, 2>), groups, dim3(256), 0, st, a);
