@@ -37,6 +37,19 @@ def _ints(t, name, dims):
     return t
 
 
+def _counts(values, name, most=2 ** 31 - 1):
+    """A ctypes array of host numbers (which by itself would take any modulo 2^32)."""
+    values = [int(n) for n in values]
+    if values and not 0 <= min(values) <= max(values) <= most:
+        raise ValueError(f"{name}: need numbers from 0 to {most}")
+    return (C.c_int32 * max(len(values), 1))(*values)
+
+
+def _check_scratch(t):
+    if not (t.is_cuda and t.is_contiguous()):
+        raise TypeError("workspace: need a contiguous CUDA tensor")
+
+
 def _heads(t, name, tokens, heads, D, dtype):
     """[tokens, heads (0: any), D] whose heads follow one another; the tokens may be strided (views of a fused projection).  Returns the distance of two tokens."""
     shape, stride = t.shape, t.stride()
@@ -92,7 +105,8 @@ class PagedStep:
         _ints(table, "table", 2)
         if table.shape[0] != B:
             raise ValueError("table needs one row per sequence")
-        self.n_tokens = int(sum(n_tok))
+        past, tok = _counts(n_past, "n_past"), _counts(n_tok, "n_tok", TREE_MAX_TOK)
+        self.n_tokens = sum(tok)
         if tree is not None:
             if not (tree.is_cuda and tree.dtype == torch.int64 and tree.is_contiguous()):
                 raise TypeError("tree: need a contiguous CUDA tensor of torch.int64")
@@ -101,9 +115,9 @@ class PagedStep:
         if positions is not None and _ints(positions, "positions", 1).numel() != self.n_tokens:
             raise ValueError("positions needs one entry per token")
         self.n_seqs = B
-        self._keep = (table, tree, positions, (C.c_int32 * max(B, 1))(*[int(n) for n in n_past]), (C.c_int32 * max(B, 1))(*[int(n) for n in n_tok]))
+        self._keep = (table, tree, positions, past, tok)
         ip = C.POINTER(C.c_int32)
-        self._step = _ffi.PagedStep(B, table.shape[1], C.cast(self._keep[3], ip), C.cast(self._keep[4], ip), table.data_ptr(),
+        self._step = _ffi.PagedStep(B, table.shape[1], C.cast(past, ip), C.cast(tok, ip), table.data_ptr(),
                                     None if tree is None else tree.data_ptr(), None if positions is None else positions.data_ptr())
         self._ref = C.byref(self._step)
         self._scratch = {}
@@ -195,8 +209,10 @@ def tree_attn(cache, layer, step, q, o=None, scale=None, workspace=None):
             workspace = q.new_empty(max(256, lib.prima_tree_attn_workspace_bytes(cache._refs[layer], step._ref, heads)), dtype=torch.uint8)
             if not capturing:
                 step._scratch[key] = workspace
+    else:
+        _check_scratch(workspace)
     code = lib.prima_tree_attn(cache._refs[layer], step._ref, heads, _DTYPES[dtype], q.data_ptr(), ldq, cache.scale if scale is None else scale, o.data_ptr(), ldo,
-                               workspace.data_ptr(), workspace.numel(), stream)
+                               workspace.data_ptr(), workspace.nbytes, stream)
     if code:
         raise PrimaError(code, "prima_tree_attn")
     return o
@@ -235,13 +251,17 @@ def beam_select(logits, scores, n_best=None, done=None, eos=0, workspace=None):
     if done is not None and not (done.is_cuda and done.dtype in (torch.uint8, torch.bool) and done.shape == scores.shape and done.is_contiguous()):
         raise TypeError("done: need a contiguous CUDA tensor of uint8 like scores")
     K, lib = W if n_best is None else n_best, _ffi.lib()
+    if not (-2 ** 31 <= eos < 2 ** 31 and K < 2 ** 31):
+        raise ValueError("eos and n_best need to be 32-bit numbers")
     if workspace is None:
         workspace = scores.new_empty(max(256, lib.prima_beam_select_workspace_bytes(B, W, V, K)), dtype=torch.uint8)
+    else:
+        _check_scratch(workspace)
     out = scores.new_empty((B, max(K, 0)))
     beams, tokens = torch.empty_like(out, dtype=torch.int32), torch.empty_like(out, dtype=torch.int32)
     code = lib.prima_beam_select(_DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if rows > 1 else V, B, W, V, scores.data_ptr(),
                                  None if done is None else done.data_ptr(), eos, K, out.data_ptr(), beams.data_ptr(), tokens.data_ptr(),
-                                 workspace.data_ptr(), workspace.numel(), _stream(scores))
+                                 workspace.data_ptr(), workspace.nbytes, _stream(scores))
     if code:
         raise PrimaError(code, "prima_beam_select")
     return out, beams, tokens
@@ -260,7 +280,7 @@ def beam_reorder(cache, table, parents, n_rows, out=None):
         out = torch.empty_like(table)
     elif _ints(out, "out", 2).shape != table.shape:
         raise ValueError("out: need a tensor like table")
-    code = _ffi.lib().prima_beam_reorder(cache._refs[0], cache.layer_stride, cache.n_layers, B, W, (C.c_int32 * max(B, 1))(*n_rows), parents.data_ptr(),
+    code = _ffi.lib().prima_beam_reorder(cache._refs[0], cache.layer_stride, cache.n_layers, B, W, _counts(n_rows, "n_rows"), parents.data_ptr(),
                                          table.data_ptr(), out.data_ptr(), width, _stream(table))
     if code:
         raise PrimaError(code, "prima_beam_reorder")
