@@ -533,7 +533,8 @@ size_t prima_beam_select_workspace_bytes(int32_t n_seqs, int32_t n_beams, int64_
  *   pages that are full: the parent's; pages behind the rows: beam w's own, as before;
  *   the partly filled page, if there is one: of the beams with one parent the lowest keeps the parent's page, each of the others gets its rows copied, in
  *   all layers, into the page of a beam that nobody continues (there are as many; both in ascending order).
- * So every beam needs a partly filled page of its own (its content does not matter before the first choice out of one beam), and none is ever short of one.
+ * So every beam needs a partly filled page of its own (its content does not matter before the first choice out of one beam), and none is ever short of one.  Pages that no row of
+ * table_out names any more are the caller's again: nothing here keeps count of them.
  * table, table_out: DEVICE [n_seqs*n_beams][table_stride], table_out must not overlap table.  n_rows: HOST array, read before the call returns.
  * Layers as in prima_tree_accept.  1 <= n_seqs <= PRIMA_PAGED_MAX_SEQS, 1 <= n_beams <= PRIMA_BEAM_MAX.
  */

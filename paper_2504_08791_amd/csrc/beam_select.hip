@@ -8,7 +8,8 @@
 // Where more elements than fit reach a threshold (many equal ones, or rows in order of their logits) the best are taken out one by one, or, of a whole workgroup, the threshold is
 // raised by counting.
 // Measured: 16 searches of 8 beams over 128256 fp32 logits (65.7 MB) 20.5 us, some 14.5 of them the first launch at 4.5 TB/s (vector units: an exponential, a maximum, a comparison
-// and a ballot a logit; its last wave ranks alone), the rest latencies of one workgroup a search; one of 4 beams over 32000 8.7; 4 of 16 over 151936 19.6.
+// and a ballot a logit; its last wave ranks alone), the rest latencies of one workgroup a search; one of 4 beams over 32000 8.2; 4 of 16 over 151936 19.1.  16-bit
+// logits are no faster (20.7): what a logit costs the vector units does not halve with its bytes.
 // Rounding: x - log sum exp x and the sum with the beam's score never reorder logits but may make two of them equal, and then the lower token comes
 // first, though a workgroup may have kept the other.  That needs a list all of whose elements are chosen or tie with the last one chosen: it has one more than can be
 // chosen, and where even that one ties, its logits are read again for tokens of exactly that score.
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(64 * SCAN_WAVES, E == 32 ? 6 : 8) beam_scan_ke
     }
 
     // what reaches the workgroup's threshold, in any order.  (Among the maxima of 256 lanes it is one that few more than are to be kept reach; each wave's own, among 64, three times as
-    // many.)
+    // many.  us of both launches, a wave's / the workgroup's: 4 searches of 16 beams over 151936 fp32 logits 20.7 / 19.1, 16 of eight over 128256 20.8 / 19.9, 2 of 32 25.0 / 22.7; 16-bit
+    // logits with few to keep wait for the barrier: 16 of eight over 128256 19.9 / 20.7, bfloat16 20.5 / 21.7, 64 of four over 32000 12.5 / 13.0 and 13.0 / 13.8.)
     maxima[threadIdx.x] = ordered(most);
     __syncthreads();
     uint32_t keys[SCAN_WAVES], largest = 0;
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(BeamArgs a)
         return w * a.V + k.token;
     };
     auto candidate = [&](int at, float &score) { return candidate_of(at, at / (a.nc * a.keep), kept[at], score); };
-    const unsigned inverse = 0xffffffffu / static_cast<unsigned>(a.nc * a.keep) + 1; // (at nc keep < 2^32: the high word of the product is the quotient; 0 for one beam)
+    const unsigned inverse = 0xffffffffu / static_cast<unsigned>(a.nc * a.keep) + 1; // (at nc keep < 2^32: the high word of the product is the quotient)
     float most = -INFINITY, held_score[HELD];
     int held_flat[HELD];
     if (held) {
@@ -533,8 +535,9 @@ static int beam_keep(int n_best) { return n_best < PRIMA_BEAM_MAX ? n_best + 1 :
 // Logits a lane takes.  32, or
 //  8 where that leaves fewer than two workgroups a compute unit (one search of four beams over 32000 tokens: 16 or 64 workgroups), unless the lists, four times as many, are
 //    then more than the second launch holds in registers;
-//  16 of 16-bit logits, which come in half the time, so that loads of some waves run beside the exponentials of others, as long as the lists are few (16 searches of eight beams over
-//    128256 binary16 logits 23.2 -> 19.8 us; fp32 21.3 and 21.6; 4 searches of 16 beams over 151936, 10336 candidates each, 19.5 -> 26.7).
+//  16 of 16-bit logits, which come in half the time, so that loads of some waves run beside the exponentials of others, as long as the lists are few (us of both launches, 32 / 16: 16
+//    searches of eight beams over 128256 binary16 logits 22.7 / 20.7, bfloat16 23.1 / 21.7, 64 of four over 32000 14.0 / 13.0 and 14.8 / 13.8, but 24 of four over 151936 15.8 / 16.8 and
+//    16.2 / 16.9; before there was one threshold a workgroup: fp32 21.3 and 21.6; 4 searches of 16 beams over 151936, 10336 candidates each, 19.5 -> 26.7).
 static int beam_lane_logits(int dtype, int n_seqs, int n_beams, int64_t vocab, int n_best)
 {
     auto candidates = [&](int E) { return n_beams * ((vocab + 64 * SCAN_WAVES * E - 1) / (64 * SCAN_WAVES * E)) * beam_keep(n_best); };

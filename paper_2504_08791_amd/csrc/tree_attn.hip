@@ -16,9 +16,9 @@
 //  * Tiles with drafted rows, rows past the end or rows whose page is absent are special: scores are masked by selection, and V's rows that nobody sees are
 //    zeroed in LDS (zero times what they hold need not be zero).  A drafted row that somebody sees and another does not may hold infinities or NaN: such elements are
 //    zeroed for the product and added to the sums of those that see them in the end.
-// Measured, with the join: one token behind 512 rows (32 / 8 heads of 128, fp32) 9.8 us, behind 30001 (64 / 8) 26.6: 4.6 TB/s, 5.1 within its launch, of which 3.5 us pass
-// before rows arrive; 16 sequences of one token behind 4100 (40 / 8, f16) 43.7: 5.3; 12 tokens behind 8192 (32 / 8, fp32) 20.9; 8 x 63 behind 6000 (64 / 8, bf16) 99: 730 TFLOP/s
-// within its launch of 1174 that a large product reaches, fp32 154.
+// Measured, with the join: one token behind 512 rows (32 / 8 heads of 128, fp32) 9.7 to 11.4 us, behind 30001 (64 / 8) 27.0: 4.6 TB/s, 5.1 within its launch, of which 3.5 us pass
+// before rows arrive; 16 sequences of one token behind 4100 (40 / 8, f16) 44.7: 5.2; 12 tokens behind 8192 (32 / 8, fp32) 21.2; 8 x 63 behind 6000 (64 / 8, bf16) 100: 730 TFLOP/s
+// within its launch of 1174 that a large product reaches, fp32 160.
 #include <atomic>
 #include <cstddef>
 #include <type_traits>
@@ -635,7 +635,7 @@ __global__ void __launch_bounds__(512, 2) tree_wide_kernel(TreeAttnArgs a)
             ls[wave * 32 + col] = l;
         }
         __syncthreads();
-    const int n = n_q - q_first;
+        const int n = n_q - q_first;
         for (int idx = threadIdx.x; idx < n * (D / 4); idx += 512) {
             const int i = idx / (D / 4), d = (idx - i * (D / 4)) * 4;
             float mx = -INFINITY, sum = 0.f;
@@ -1133,15 +1133,15 @@ static TreePlan tree_plan(const PagedArgs &p, int Hq, int D, bool split, TreeAtt
     if (most_tok == 0) return r;
     const int most_q = most_tok * G, places_narrow = 512, places_wide = 256; // workgroups that run at once
     // More than 32 queries on a head: the narrow kernel brings the rows once for every 32 of them, the wide one up to 256, but with eight waves and barriers.
-    // us, narrow / wide, one sequence, 8 KV heads: 48 fp32 queries behind 1000 rows 13.2 / 16.7, 8192: 20.8 / 22.0, 16000: 26.6 / 24.4; 96: 4000 19.2 / 21.0,
-    // 8192 25.2 / 24.4; 504 bf16 queries 1000: 19.4 / 22.4, 4000: 36.5 / 30.2; eight sequences of 48 behind 1000: 21.0 / 22.4, 2000: 33.3 / 24.8.
-    // And up to 64 queries of more sequences than the wide kernel has places for, behind few rows: 64 of 8 fp32 tokens, 64 / 8 heads, behind 200 rows 29.1 / 36.0, 500 47.0 / 50.7,
-    // 1000 73.2 / 70.0; 41 of 16, 32 / 8 heads, behind 119 21.1 / 29.7.
+    // us, narrow / wide, one sequence, 8 KV heads: 48 fp32 queries behind 1000 rows 13.2 / 17.5, 8192: 21.2 / 22.7, 16000: 27.0 / 24.9; 96: 4000 19.4 / 21.1,
+    // 8192 25.3 / 25.0; 504 bf16 queries 1000: 19.3 / 19.3, 4000: 39.2 / 26.5; eight sequences of 48 fp32 queries behind 1000: 20.9 / 21.8, 2000: 24.8 / 24.0.
+    // And up to 64 queries of more sequences than the wide kernel has places for, behind few rows: 64 of 8 fp32 tokens, 64 / 8 heads, behind 200 rows 29.4 / 35.9, 500 44.9 / 50.4,
+    // 1000 73.4 / 66.9 (bf16 25.1 / 27.8, 40.8 / 39.4, 62.3 / 56.3); 41 of 16, 32 / 8 heads, behind 119 20.7 / 27.3.
     if (most_q <= 32 || (pieces <= places_narrow && work <= 200000) || (most_q <= 64 && pieces_64 > places_wide && work <= 512 * pieces)) r.narrow = most_q <= 16 ? 1 : 2;
     // More than 128: eight waves of queries, which bring the rows half as often as four and another four for other rows; four where the ranges of eight would be short (660 rows and
     // fewer) and their records many, unless they are more than run at once, and for fp32 queries, for which eight leave registers short.  us, four / eight, 64 / 8 heads: one sequence of
-    // 20 bf16 tokens behind 8000 rows 22.9 / 25.7, 32000 51.4 / 46.4, 63 behind 4000 26.7 / 31.2, eight of 63 behind 1000 33.7 / 35.1, 4000 86.1 / 75.2, 16 of 40 behind 1000 47.3 / 38.4;
-    // fp32 27.1 / 32.4, 64.0 / 70.9, 32.8 / 38.3, 41.8 / 47.0, 113 / 117, 60.4 / 58.9.
+    // 20 bf16 tokens behind 8000 rows 22.8 / 25.8, 32000 50.7 / 47.2, 63 behind 4000 26.4 / 31.2, eight of 63 behind 1000 33.1 / 34.9, 4000 83.6 / 75.9, 16 of 40 behind 1000 46.9 / 38.3;
+    // fp32, when it had eight, 27.1 / 32.4, 64.0 / 70.9, 32.8 / 38.3, 41.8 / 47.0, 113 / 117, 60.4 / 58.9.
     else r.wide = most_q <= 64 ? 2 : (most_q <= 128 || split || (work_256 <= 660 * places_wide && pieces_128 <= places_wide) ? 4 : 8);
     const int tile_q = r.narrow ? 16 * r.narrow : 32 * r.wide;
     const int q_tiles = (most_q + tile_q - 1) / tile_q;
